@@ -429,9 +429,10 @@ nvfp4_status nvfp4_gdn_lockstep(const float* d_q, const float* d_k, const float*
  *     g_t = -exp(A_log[h]) * softplus(a_t + dt_bias[h]);  alpha_t = exp(g_t);  beta_t = sigmoid(b_t)
  *     S_t = alpha_t S_{t-1} + beta_t k_t (v_t - kappa_t S_{t-1}^T k_t)^T;   o_t = S_t^T (q_t / sqrt(128))
  * kappa_t = 1 as in Eq. 2 (and in nvfp4_gdn_lockstep), or alpha_t with NVFP4_GDN_DECAY_FIRST: the prediction then
- * reads the decayed state, the form most published models use.  States are binary32 and everything that reaches them is
- * formed to binary32 accuracy; so are float outputs and those of nvfp4_gdn_decode.  nvfp4_gdn_prefill with bf16 output reads
- * out on fp16 operands (2^-12 relative each, below the output's own 2^-9).  Outputs are rounded once.
+ * reads the decayed state, the form most published models use.  States are binary32 and so are all
+ * sums.  nvfp4_gdn_decode multiplies in binary32; nvfp4_gdn_prefill multiplies operands of 22 significant bits (two fp16 each;
+ * what is less than 2^-15 of the largest value of its row in a chunk of 64 tokens keeps 2^-37 of that value), which leaves about
+ * three times the error of a binary32 evaluation.  Outputs of either type are formed alike and rounded once.
  *
  * Flags of the two calls:
  *   NVFP4_OUT_F32          o is float instead of bf16

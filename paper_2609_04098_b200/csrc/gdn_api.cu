@@ -108,10 +108,10 @@ nvfp4_status launch_gdn_chunks(const GdnParams& p, const GdnWorkspace& w, bool e
 
 extern "C" {
 
-size_t nvfp4_gdn_prefill_workspace_bytes(int64_t T, int64_t nseq, int Hk, int Hv, uint32_t flags) {
+size_t nvfp4_gdn_prefill_workspace_bytes(int64_t T, int64_t nseq, int Hk, int Hv, uint32_t /* flags: no part of it so far */) {
     if (T < 0 || nseq < 0 || Hk < 1 || Hv < 1) return 0;
     return kStatusBytes + gdn_kq_bytes(T, nseq, Hk) +
-           static_cast<size_t>(gdn_chunk_slots(T, nseq)) * static_cast<size_t>(Hv) * gdn_tp_bytes((flags & NVFP4_OUT_F32) != 0u);
+           static_cast<size_t>(gdn_chunk_slots(T, nseq)) * static_cast<size_t>(Hv) * kGdnTpBytes;
 }
 
 nvfp4_status nvfp4_gdn_prefill(const void* d_q, int64_t ldq, const void* d_k, int64_t ldk, const void* d_v, int64_t ldv,

@@ -9,11 +9,11 @@
 // T and P depend on no state: gdn_chunk_prepare_kernel computes them for all chunks in parallel.  What is serial is
 // gdn_chunk_kernel, one CTA per (sequence, value head) walking the chunks with S in registers.
 //
-// What bounds it (B200, 16 key and 48 value heads).  One 8192-token prompt takes 553 us against 41 us for its bytes (32 KB a
-// token) and about 50 us for its arithmetic: 128 chunks one after the other at 3.6 us alone and 4.1 us beside the preparation
+// What bounds it (B200, 16 key and 48 value heads).  One 8192-token prompt takes 578 us against 41 us for its bytes (32 KB a
+// token) and about 50 us for its arithmetic: 128 chunks one after the other at 3.6 us alone and 4.3 us beside the preparation
 // of the next range, of which the tensor cores work about a fifth -- the rest is the way of S, R and U out of accumulators,
 // through a scale, a split and back (conversions and maxima, which share the schedulers, and six barrier hops).  16 prompts of
-// 16001 tokens (float output): 646 us, 229 of them the preparation, against 124 us for their bytes.  Beside its chunks a CTA
+// 16001 tokens (float output): 640 us, 229 of them the preparation, against 124 us for their bytes.  Beside its chunks a CTA
 // costs about 9 us (set-up 1, state 2, first tiles 2, last output 1, state out 1, next CTA 1.5); asking for the state in front
 // of the set-up, for the first tiles in front of it, or storing the state in front of the last output all measured slower
 // (up to 3 us a CTA: the two then share one burst of loads).  The same serial part on mma.sync with S
@@ -24,8 +24,9 @@
 // Precision.  The products run on fp16 operands with binary32 accumulation, but to binary32 accuracy: an operand that is not
 // a bf16 input is split into hi + lo fp16 (22 bits) after a power-of-two scale that puts its row's largest value at 2^12;
 // keys and queries are exact in one fp16 (8 significant bits, scaled by a power of two per token; what is 2^-24 of a token's
-// largest element or less flushes).  Products keep hi*hi + hi*lo + lo*hi.  bf16 output drops lo terms that only it would see
-// (2^-12 relative against its own 2^-9).  The chunk's update is summed in a fresh accumulator and added to S with one rounded
+// largest element or less flushes).  Products keep hi*hi + hi*lo + lo*hi, those of the read-out too, whatever the output's type: where
+// q.S and P U cancel, an operand rounded to 11 bits would show in front of bf16's own rounding (it would save 26 of the 578 us).
+// The chunk's update is summed in a fresh accumulator and added to S with one rounded
 // fma, so the tensor core's own rounding of running sums does not pile up over a long prompt.
 #pragma once
 #include <cstddef>
@@ -50,14 +51,14 @@ constexpr int kGdnVecT = 196, kGdnVecP = 200;
 // because ceil(len / 64) <= (begin + len) / 64 - begin / 64 + 1), so no prefix sum over the sequences is needed
 struct GdnWorkspace {
     uint8_t* kq;            // [slot][Hk][2][64 x 128 fp16], swizzled tiles
-    uint8_t* tp;            // [slot][Hv][T hi | T lo | P hi (| P lo) | vec]
+    uint8_t* tp;            // [slot][Hv][T hi | T lo | P hi | P lo | vec]
     uint32_t* status;
     uint64_t wait_limit_ns;
     // the chunks of every sequence that a launch handles: [chunk_begin, chunk_begin + chunk_count); 0: all of them
     int32_t chunk_begin, chunk_count;
     uint32_t sm_count;
 };
-__host__ __device__ constexpr int gdn_tp_bytes(bool out_f32) { return (out_f32 ? 4 : 3) * kGdnSquareBytes + kGdnVecBytes; }
+constexpr int kGdnTpBytes = 4 * kGdnSquareBytes + kGdnVecBytes;
 
 __device__ __forceinline__ int gdn_first_slot(const GdnParams& p, int seq) { return min(max(p.cu[seq], 0), p.T) / kGdnChunk + seq; }
 
@@ -209,7 +210,6 @@ gdn_chunk_prepare_kernel(const __grid_constant__ GdnParams p, const __grid_const
     GdnPrepSmem& sm = *reinterpret_cast<GdnPrepSmem*>(prep_raw);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int h0 = blockIdx.y * heads_per_cta;
-    const bool out_f32 = (p.flags & NVFP4_OUT_F32) != 0u;
     ptx::pdl_launch_dependents();                           // (the serial kernel: it waits for this grid's end)
     int seq = 0, slot = blockIdx.x;
     if (w.chunk_count != 0) {                               // one range of chunks of every sequence
@@ -398,8 +398,8 @@ gdn_chunk_prepare_kernel(const __grid_constant__ GdnParams p, const __grid_const
             }
         }
         __syncthreads();                                    // the gates are in place
-        uint8_t* dst = w.tp + (static_cast<int64_t>(slot) * p.Hv + h) * gdn_tp_bytes(out_f32);
-        float* const vec = reinterpret_cast<float*>(dst + (out_f32 ? 4 : 3) * kGdnSquareBytes);
+        uint8_t* dst = w.tp + (static_cast<int64_t>(slot) * p.Hv + h) * kGdnTpBytes;
+        float* const vec = reinterpret_cast<float*>(dst + 4 * kGdnSquareBytes);
         if (tid < kGdnChunk) {
             const float Gc = gt.Gh[kGdnChunk - 1];
             vec[tid] = exp2f(gt.Eh[tid]) * sm.rho[tid];
@@ -450,7 +450,7 @@ gdn_chunk_prepare_kernel(const __grid_constant__ GdnParams p, const __grid_const
         };
         // a strip, split, to the chunk's squares: blocks on and below the diagonal only (nothing reads the others), each block
         // of 16 rows with its own scale
-        auto store_strip = [&](const float (&x)[6][4], const float (&diag)[2][4], uint8_t* to, bool with_lo, float* inv_at) {
+        auto store_strip = [&](const float (&x)[6][4], const float (&diag)[2][4], uint8_t* to, float* inv_at) {
             float m = 0.0f;
 #pragma unroll
             for (int e = 0; e < 4; e += 2) m = gdn_max_abs(gdn_max_abs(m, diag[0][e], diag[0][e + 1]), diag[1][e], diag[1][e + 1]);
@@ -470,7 +470,7 @@ gdn_chunk_prepare_kernel(const __grid_constant__ GdnParams p, const __grid_const
                     uint32_t vh, vl;
                     gdn_split(v[e], v[e + 1], sc, vh, vl);
                     *reinterpret_cast<uint32_t*>(at) = vh;
-                    if (with_lo) *reinterpret_cast<uint32_t*>(at + kGdnSquareBytes) = vl;
+                    *reinterpret_cast<uint32_t*>(at + kGdnSquareBytes) = vl;
                 }
             };
             store_tile(diag[0], 2 * warp);
@@ -482,7 +482,7 @@ gdn_chunk_prepare_kernel(const __grid_constant__ GdnParams p, const __grid_const
             }
         };
         decays(qk, qd, false);
-        store_strip(qk, qd, dst + 2 * kGdnSquareBytes, out_f32, vec + kGdnVecP);
+        store_strip(qk, qd, dst + 2 * kGdnSquareBytes, vec + kGdnVecP);
         decays(kk, kd, true);
         // ---- D_w: lanes 0..15 and 16..31 both walk the block's columns; the first half stores hi, the second lo
         float T[6][4], Td[2][4];
@@ -609,7 +609,7 @@ gdn_chunk_prepare_kernel(const __grid_constant__ GdnParams p, const __grid_const
             if (t >= 2 * warp) break;
             times_beta(T[t], t);
         }
-        store_strip(T, Td, dst, true, vec + kGdnVecT);
+        store_strip(T, Td, dst, vec + kGdnVecT);
     }
     if (tid == 0) ptx::bulk_wait_group_read<0>();
     if (last_out) ptx::pdl_wait();
@@ -632,7 +632,7 @@ gdn_chunk_prepare_kernel(const __grid_constant__ GdnParams p, const __grid_const
 template <bool F32>
 struct GdnChunkCfg {
     static constexpr int STAGES = 2;
-    static constexpr int TP_BYTES = gdn_tp_bytes(F32);
+    static constexpr int TP_BYTES = kGdnTpBytes;
     static constexpr int V_BYTES = kGdnChunk * kGdnWidth * 2;
     static constexpr int KQ_OFF = 0;                                   // 1024-byte aligned, as T and P behind it
     static constexpr int TP_OFF = 2 * kGdnTileBytes;
@@ -846,12 +846,10 @@ gdn_chunk_kernel(const __grid_constant__ GdnParams p, const __grid_constant__ Gd
             if (!ok) break;
             ptx::tc_fence_after();
             product(tmem + kTmQ, tmem + kTmSh, q_d, 1u);
-            if (F32) product(tmem + kTmQ, tmem + kTmSl, q_d, 0u);
+            product(tmem + kTmQ, tmem + kTmSl, q_d, 0u);
             lower(tmem + kTmY, tmem + kTmX, p_d, 1u);
-            if (F32) {
-                lower(tmem + kTmY, tmem + kTmX + 16, p_d, 0u);
-                lower(tmem + kTmY, tmem + kTmX, p_d + (kGdnSquareBytes >> 4), 0u);
-            }
+            lower(tmem + kTmY, tmem + kTmX + 16, p_d, 0u);
+            lower(tmem + kTmY, tmem + kTmX, p_d + (kGdnSquareBytes >> 4), 0u);
             ptx::tc_commit_if(y_full, lp);
             ptx::tc_commit_if(&empty[s], lp);
         }
@@ -1055,17 +1053,9 @@ gdn_chunk_kernel(const __grid_constant__ GdnParams p, const __grid_constant__ Gd
                 gdn_pow2_scale(m, 12, su, iu);
                 gdn_pow2_scale(wm, 12, sw, iw);
                 uint32_t hi[16], lo[16];
-                if (F32) {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) gdn_split(u[2 * i], u[2 * i + 1], su, hi[i], lo[i]);
-                    ptx::tmem_st_32x16(tq + kTmX + 32 * half + 16, lo);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        gdn_mul2(u[2 * i], u[2 * i + 1], su, su);
-                        hi[i] = gdn_half2(u[2 * i], u[2 * i + 1]);
-                    }
-                }
+                for (int i = 0; i < 16; ++i) gdn_split(u[2 * i], u[2 * i + 1], su, hi[i], lo[i]);
+                ptx::tmem_st_32x16(tq + kTmX + 32 * half + 16, lo);
                 ptx::tmem_st_32x16(tq + kTmX + 32 * half, hi);
 #pragma unroll
                 for (int i = 0; i < 16; ++i) gdn_split(r[2 * i], r[2 * i + 1], sw, hi[i], lo[i]);
