@@ -321,8 +321,8 @@ size_t nvfp4_linear_bf16_workspace_bytes(int64_t M, int64_t N, int64_t K, int ns
  *   d_bias        optional (NULL: none): bf16 [N], 16-byte aligned
  *   activation    nvfp4_activation
  *   d_residual    optional (NULL: none): [M, N] of the output's type (bf16; float with NVFP4_OUT_F32), row stride ldr >= N
- *                 elements.  It may be Y itself (same address, ldr == ldy: the residual stream updated in place); any other
- *                 overlap with Y is NVFP4_ERR_SHAPE, except columns of one buffer side by side
+ *                 elements.  It may be Y itself (same address, and ldr == ldy where M > 1: the residual stream updated
+ *                 in place); any other overlap with Y is NVFP4_ERR_SHAPE, except columns of one buffer side by side
  * Y must not overlap d_x (NVFP4_ERR_SHAPE) unless they are columns of one buffer side by side.
  * epilogue == NULL, or one without any of the three, is nvfp4_linear / nvfp4_linear_bf16.  Everything else -- operands, workspace,
  * flags, in-kernel quantization of a few rows, errors -- is as for those two.

@@ -1029,8 +1029,8 @@ nvfp4_status check_epilogue(const nvfp4_epilogue* epi, int64_t M, int64_t N, con
         const uintptr_t r = reinterpret_cast<uintptr_t>(epi->d_residual);
         if (epi->ldr < N) return NVFP4_ERR_SHAPE;
         if (r % static_cast<uintptr_t>(es) != 0) return NVFP4_ERR_ALIGN;
-        // Y itself is fine: every element is read by the thread that writes it
-        if (!(epi->d_residual == d_y && epi->ldr == ldy) && ldy >= N &&
+        // Y itself is fine: every element is read by the thread that writes it (a single row is Y itself whatever the strides)
+        if (!(epi->d_residual == d_y && (epi->ldr == ldy || M <= 1)) && ldy >= N &&
             blocks_overlap(epi->d_residual, epi->ldr * es, N * es, d_y, ldy * es, N * es, M))
             return NVFP4_ERR_SHAPE;
         out->residual = epi->d_residual;
