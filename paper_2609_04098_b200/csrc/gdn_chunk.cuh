@@ -304,7 +304,9 @@ gdn_chunk_prepare_kernel(const __grid_constant__ GdnParams p, const __grid_const
         const bool l2 = (p.flags & NVFP4_GDN_L2NORM) != 0u;
         auto factor = [&](float* f, int r, float ss, float extra) {
             const float s = f[r];
-            f[r] = r < n ? extra * (l2 ? 1.0f / sqrtf(ss + kGdnL2Eps * s * s) : 1.0f / s) : 0.0f;      // rows that are not there: 0
+            // from s = 2^48 on (a row below 2^-37) the sum, at most 2^29, is below 2^-47 of the epsilon and s * s may overflow
+            const float length = s < 0x1p48f ? sqrtf(ss + kGdnL2Eps * s * s) : sqrtf(kGdnL2Eps) * s;
+            f[r] = r < n ? extra * (1.0f / (l2 ? length : s)) : 0.0f;                                  // rows that are not there: 0
         };
         if ((g8 >> 1) == (lane & 3)) {                      // this lane holds the diagonal's rows g8 and g8 + 8
             const int odd = g8 & 1;
