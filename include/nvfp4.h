@@ -467,7 +467,9 @@ nvfp4_status nvfp4_gdn_lockstep(const float* d_q, const float* d_k, const float*
  *                not read; else it continues from the slot's state.  The final state goes to the slot either way
  *   d_workspace  nvfp4_gdn_prefill_workspace_bytes(...) bytes, 256-byte aligned, with a status block in front like every
  *                workspace of this library (nvfp4_workspace_reset before the first use, nvfp4_device_status).
- *                Calls that may overlap on the GPU, captured graphs among them, need one each
+ *                Calls that may overlap on the GPU, captured graphs among them, need one each.  After NVFP4_ERR_TIMEOUT in its
+ *                status o is void, and the state of a head is whole: the one from before the call, from behind it or, of a
+ *                long prompt, from a place in between
  * Errors: NULL, shapes (T, nseq, nslots < 0, nseq > 65535, Hv > 65535, Hv % Hk), alignment, workspace.
  */
 nvfp4_status nvfp4_gdn_prefill(const void* d_q, int64_t ldq, const void* d_k, int64_t ldk, const void* d_v, int64_t ldv,

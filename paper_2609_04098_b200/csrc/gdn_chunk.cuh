@@ -665,17 +665,18 @@ __device__ __forceinline__ void gdn_mma_ts(uint32_t d, uint32_t a, uint32_t b_lo
         ::"r"(d), "r"(a), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate), "r"(pred)
         : "memory");
 }
-// barrier of the 64 threads that share 32 rows; true where all of them pass true
-__device__ __forceinline__ bool gdn_pair_barrier(int id, bool ok) {
+// barrier of THREADS threads; true where all of them pass true
+template <int THREADS>
+__device__ __forceinline__ bool gdn_and_barrier(int id, bool ok) {
     uint32_t r;
     asm volatile(
         "{\n\t"
         ".reg .pred p, q;\n\t"
         "setp.ne.b32 p, %2, 0;\n\t"
-        "barrier.cta.red.and.pred q, %1, 64, p;\n\t"
+        "barrier.cta.red.and.pred q, %1, %3, p;\n\t"
         "selp.u32 %0, 1, 0, q;\n\t"
         "}\n"
-        : "=r"(r) : "r"(id), "r"(static_cast<uint32_t>(ok)) : "memory");
+        : "=r"(r) : "r"(id), "r"(static_cast<uint32_t>(ok)), "n"(THREADS) : "memory");
     return r != 0u;
 }
 
@@ -874,7 +875,7 @@ gdn_chunk_kernel(const __grid_constant__ GdnParams p, const __grid_constant__ Gd
         auto exchange = [&](int which, float m, bool ok_in, bool& ok_out) {
             float* slot = mx + which * (2 * kGdnWidth);
             slot[half * kGdnWidth + row] = m;
-            ok_out = gdn_pair_barrier(1 + (warp & 3), ok_in);
+            ok_out = gdn_and_barrier<64>(1 + (warp & 3), ok_in);          // (the two warps that share 32 rows)
             return fmaxf(m, slot[(half ^ 1) * kGdnWidth + row]);
         };
         // O of chunk c, 16 of this warp's 32 tokens (part 0 or 1), from S^T Q^T and U^T P^T: it leaves beside the products of the
@@ -942,7 +943,10 @@ gdn_chunk_kernel(const __grid_constant__ GdnParams p, const __grid_constant__ Gd
             for (int i = 0; i < 64; i += 2) m = gdn_max_abs(m, S[i], S[i + 1]);
             bool both;
             m = exchange(0, m, ok, both);
-            if (!both) break;                                    // (the two warps of these rows leave together)
+            if (!both) {                                         // (the two warps of these rows leave together)
+                ok = false;
+                break;
+            }
             float sc, is;
             gdn_pow2_scale(m, 12, sc, is);
             {
@@ -1049,7 +1053,7 @@ gdn_chunk_kernel(const __grid_constant__ GdnParams p, const __grid_constant__ Gd
                 float* slot2 = mx + 3 * (2 * kGdnWidth);
                 slot[half * kGdnWidth + row] = m;
                 slot2[half * kGdnWidth + row] = wm;
-                gdn_pair_barrier(1 + (warp & 3), true);
+                gdn_and_barrier<64>(1 + (warp & 3), true);
                 m = fmaxf(m, slot[(half ^ 1) * kGdnWidth + row]);
                 wm = fmaxf(wm, slot2[(half ^ 1) * kGdnWidth + row]);
                 gdn_pow2_scale(m, 12, su, iu);
@@ -1094,12 +1098,15 @@ gdn_chunk_kernel(const __grid_constant__ GdnParams p, const __grid_constant__ Gd
             ok = ptx::mbar_wait_bounded(y_full, static_cast<uint32_t>(chunks - 1) & 1u, abort_flag, w.wait_limit_ns);
             ok = __all_sync(0xffffffffu, ok);
             ptx::tc_fence_after();
-            if (ok) {
+        }
+        // Every compute warp passes here once, whichever way it left the loop.  If one gave up, none writes: a head's state in the
+        // pool is the one from before or the one from behind these chunks, never some of both.
+        ok = gdn_and_barrier<256>(5, ok);
+        if (ok) {
+            if (chunks > 0) {
                 output(chunks - 1, 0, is_prev, iu_prev);
                 output(chunks - 1, 1, is_prev, iu_prev);
             }
-        }
-        if (ok) {
 #pragma unroll
             for (int i = 0; i < 64; ++i) state[i * kGdnWidth] = S[i];
         }
