@@ -157,7 +157,6 @@ __device__ __forceinline__ void st_cluster_u32(uint32_t cluster_saddr, uint32_t 
 }
 
 // ---------------------------------------------------------------- TMA
-__device__ __forceinline__ void prefetch_l2(const void* g) { asm volatile("prefetch.global.L2 [%0];" ::"l"(g)); }
 __device__ __forceinline__ void prefetch_tensormap(const CUtensorMap* m) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(m)) : "memory");
 }
