@@ -318,6 +318,7 @@ size_t nvfp4_linear_bf16_workspace_bytes(int64_t M, int64_t N, int64_t K, int ns
  * kernel): the product never goes to memory in between and is rounded once,
  *     Y[m, n] = round_out( act( acc[m, n] * g_a * g_seg[seg(n)] + bias[n] ) + residual[m, n] )     (binary32)
  * with act none, SiLU x / (1 + e^-x), GELU in its tanh form 0.5 x (1 + tanh(sqrt(2/pi) (x + 0.044715 x^3))), or ReLU.
+ * The exponential e^z and the division of SiLU and GELU are the hardware's approximations: (|z| + 4) 2^-23 relative.
  *   d_bias        optional (NULL: none): bf16 [N], 16-byte aligned
  *   activation    nvfp4_activation
  *   d_residual    optional (NULL: none): [M, N] of the output's type (bf16; float with NVFP4_OUT_F32), row stride ldr >= N
@@ -436,7 +437,8 @@ nvfp4_status nvfp4_gdn_lockstep(const float* d_q, const float* d_k, const float*
  *
  * Flags of the two calls:
  *   NVFP4_OUT_F32          o is float instead of bf16
- *   NVFP4_GDN_L2NORM       q and k are divided by their length first: x / sqrt(sum x^2 + 1e-6) (squares in binary32)
+ *   NVFP4_GDN_L2NORM       q and k are divided by their length first: x / sqrt(sum x^2 + 1e-6) (squares in binary32:
+ *                          elements below 2^60 in size)
  *   NVFP4_GDN_GATES_F32    a and b are float instead of bf16
  *   NVFP4_GDN_DECAY_FIRST  kappa_t = alpha_t
  * Arguments of the two calls:
@@ -461,7 +463,8 @@ nvfp4_status nvfp4_gdn_lockstep(const float* d_q, const float* d_k, const float*
 /*
  * Packed prompts: sequence i is tokens [d_cu_seqlens[i], d_cu_seqlens[i + 1]) of the arrays (device int32 [nseq + 1],
  * ascending, within [0, T]; they are clamped so that no access leaves the arrays, whatever they hold, but the results of
- * offsets that are not ascending are unspecified).  Tokens that belong to no sequence
+ * offsets that are not ascending are unspecified).  More than 32 sequences start in the order given; a prompt much longer than
+ * the others is best put first then.  Tokens that belong to no sequence
  * are left alone: their rows of o are not written.  An empty sequence keeps its state (or gets a zero one, see below).
  *   d_has_state  optional (NULL: all 1): uint8 [nseq]; 0: the sequence starts from S = 0 and the slot's content is
  *                not read; else it continues from the slot's state.  The final state goes to the slot either way

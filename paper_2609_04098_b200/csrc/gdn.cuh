@@ -77,11 +77,12 @@ __device__ __forceinline__ void gdn_store(void* o, int64_t at, float v, uint32_t
 
 // ------------------------------------------------------------------------------------------ single tokens
 // Bound by the state: 64 KB read and written per (sequence, value head), everything else is small.  256 sequences of 48 heads:
-// 246 us, 6.6 TB/s, the rate of a plain copy; 37 of 32: 25 us, 6.2 TB/s; one of 48: 5.8 us, latency.  (A thread per state column
+// 248 us, 6.5 TB/s, the rate of a plain copy; 37 of 32: 29 us, 5.3 TB/s (20 us replayed on one pool, part of which stays in L2);
+// one of 48: 4.2 us from memory, 3.3 us from L2, latency.  (A thread per state column
 // with 128 values in registers, the form of the lockstep study, takes 347 us, 39 us and 28 us.)  A CTA of eight warps
 // takes COLS columns of one head's state into registers in one go (a lane has float4 pieces of rows, coalesced), forms the
 // prediction S^T k (each thread its rows, then across threads), updates its pieces, writes them back and forms S^T q the same
-// way.  Two barriers; the loads of several CTAs per SM overlap each other's arithmetic and stores.
+// way.  Three barriers; the loads of several CTAs per SM overlap each other's arithmetic and stores.
 constexpr int kGdnDecodeThreads = 256;
 
 template <int COLS>

@@ -161,7 +161,9 @@ nvfp4_status nvfp4_gdn_prefill(const void* d_q, int64_t ldq, const void* d_k, in
     const int64_t slots = gdn_chunk_slots(T, nseq);
     auto prepare = [&](int64_t ctas_x, bool early) {
         // the value heads of one key head in one CTA (keys and queries converted once) when that still gives every SM
-        // several CTAs; one CTA per value head otherwise, for latency
+        // several CTAs; one CTA per value head otherwise, for latency.  16 key and 48 value heads, whole calls, one head a CTA
+        // against three: 17 tokens 17.7 and 27.0 us, 512 49.6 and 55.7, 1024 91 and 90, 2048 172 and 165, 7 prompts of 1500
+        // each 490 and 451
         const int heads = ctas_x * Hk >= 4ll * info.sm_count ? Hv / Hk : 1;
         cudaLaunchConfig_t cfg;
         std::memset(&cfg, 0, sizeof(cfg));
@@ -180,9 +182,12 @@ nvfp4_status nvfp4_gdn_prefill(const void* d_q, int64_t ldq, const void* d_k, in
     };
     auto serial = [&](bool early) { return out_f32 ? launch_gdn_chunks<true>(p, w, early, s) : launch_gdn_chunks<false>(p, w, early, s); };
     // Few long sequences leave SMs idle during the serial part: the chunks go in ranges, and the next range is prepared under
-    // the serial kernel of the current one.  8192 tokens, 48 heads: 615 us in one piece; 574 / 560 / 555 / 570 us in ranges of
-    // 16 / 24 / 32 / 48 chunks.  With every SM busy ranges only cost (16 prompts of 16001 tokens: 770 us in one piece, 990 us in
-    // ranges of 16): the preparation then takes from the serial kernel what it hides.
+    // the serial kernel of the current one.  8192 tokens, 48 heads: 624 us in one piece; 593 / 584 / 577 / 581 us in ranges of
+    // 16 / 24 / 32 / 48 chunks.  With every SM busy ranges only cost (16 prompts of 1000 tokens each, float output: 690 us in one
+    // piece, 830 us in ranges): the preparation then takes from the serial kernel what it hides.  Between half and all of the SMs
+    // it goes either way -- 96 CTAs: two prompts of 8192 730 us in one piece and 669 us in ranges, three of 4096 at 32 heads
+    // 384 and 372; 128 and 144 CTAs: four of 4096 at 32 heads 421 and 450, three at 48 heads 436 and 460 -- and the rule takes
+    // one piece.
     // Lengths are on the device: the longest sequence may have all T tokens, and a range that no sequence reaches still costs
     // its two launches, so an average length decides.
     constexpr int64_t kRange = 32;
@@ -212,7 +217,8 @@ nvfp4_status nvfp4_gdn_decode(const void* d_q, int64_t ldq, const void* d_k, int
     DeviceInfo info;
     st = check_arch(info);
     if (st != NVFP4_OK) return st;
-    // a whole head per CTA; a quarter of one while that still leaves SMs idle (few sequences: latency, not bandwidth)
+    // a whole head per CTA; a quarter of one while that still leaves SMs idle (few sequences: latency, not bandwidth).  48 heads,
+    // quarters against whole heads: 1 sequence 3.3 and 4.2 us, 3 4.5 and 5.8, 6 8.0 and 7.5, 7 9.8 and 7.9, 12 14.5 and 10.9
     const bool quarters = batch * Hv <= 2ll * info.sm_count;
     cudaLaunchConfig_t cfg;
     std::memset(&cfg, 0, sizeof(cfg));

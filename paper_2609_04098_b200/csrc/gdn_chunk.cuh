@@ -708,8 +708,10 @@ gdn_chunk_kernel(const __grid_constant__ GdnParams p, const __grid_constant__ Gd
     int seq = blockIdx.y, begin, len;
     if (gridDim.x * gridDim.y > w.sm_count && gridDim.y <= 32) {
         // More CTAs than SMs: CTAs start in the order of their index, so the longest sequence goes first and short ones fill the
-        // end.  Lane i counts the sequences in front of sequence i.  16 sequences of 100 to 1540 tokens in ascending order, 48 heads: 387 us in that order, 352 us so;
-        // six of 200 and one of 2000 behind them: 233 and 194 us.  (Among more than 32 sequences one that ends late weighs little.)
+        // end.  Lane i counts the sequences in front of sequence i.  16 sequences of 100 to 1540 tokens in ascending order, 48 heads:
+        // 543 us in that order, 506 us so; six of 200 and one of 2000 behind them: 235 and 194 us.  More than 32 sequences, one
+        // more than a lane each, start in the caller's order, and a long one behind them waits: 40 of 64 tokens and one of 8192
+        // take 802 us with the long one last and 668 us with it first.
         const int mine = static_cast<int>(lane);
         begin = 0;
         len = -1;
