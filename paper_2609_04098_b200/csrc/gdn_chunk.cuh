@@ -10,24 +10,24 @@
 // gdn_chunk_kernel, one CTA per (sequence, value head) walking the chunks with S in registers.
 //
 // What bounds it (B200, 16 key and 48 value heads).  One 8192-token prompt takes 578 us against 41 us for its bytes (32 KB a
-// token) and about 50 us for its arithmetic: 128 chunks one after the other at 3.6 us alone and 4.3 us beside the preparation
-// of the next range, of which the tensor cores work about a fifth -- the rest is the way of S, R and U out of accumulators,
-// through a scale, a split and back (conversions and maxima, which share the schedulers, and six barrier hops).  16 prompts of
-// 16001 tokens (float output): 640 us, 229 of them the preparation, against 124 us for their bytes.  Beside its chunks a CTA
-// costs about 9 us (set-up 1, state 2, first tiles 2, last output 1, state out 1, next CTA 1.5); asking for the state in front
+// token) and about 70 us for its arithmetic: 128 chunks one after the other at 3.7 us alone (4.1 us with float output) and 4.3 us
+// beside the preparation of the next range, of which the tensor cores work about a quarter -- the rest is the way of S, R and U
+// out of accumulators, through a scale, a split and back (conversions and maxima, which share the schedulers, and six barrier
+// hops).  16 prompts of 16001 tokens (float output): 640 us, 229 of them the preparation, against 124 us for their bytes.  Beside
+// its chunks a CTA costs about 9 us (set-up 1, state 2, first tiles 2, last output 1, state out 1, next CTA 1.5); asking for the state in front
 // of the set-up, for the first tiles in front of it, or storing the state in front of the last output all measured slower
 // (up to 3 us a CTA: the two then share one burst of loads).  The same serial part on mma.sync with S
 // in accumulator layout, 16 columns a warp, no barriers between the products, measured 437 us against 471 us for the single
 // prompt (each head on two SMs) and 605 us against 460 us for the batch; a separate warpgroup for the output, sixteen compute
 // warps instead of eight, and five preparation CTAs an SM instead of four (96 registers) all measured slower.
 //
-// Precision.  The products run on fp16 operands with binary32 accumulation, but to binary32 accuracy: an operand that is not
-// a bf16 input is split into hi + lo fp16 (22 bits) after a power-of-two scale that puts its row's largest value at 2^12;
-// keys and queries are exact in one fp16 (8 significant bits, scaled by a power of two per token; what is 2^-24 of a token's
-// largest element or less flushes).  Products keep hi*hi + hi*lo + lo*hi, those of the read-out too, whatever the output's type: where
-// q.S and P U cancel, an operand rounded to 11 bits would show in front of bf16's own rounding (it would save 26 of the 578 us).
-// The chunk's update is summed in a fresh accumulator and added to S with one rounded
-// fma, so the tensor core's own rounding of running sums does not pile up over a long prompt.
+// Precision.  The products run on fp16 operands with binary32 accumulation.  An operand that is not a bf16 input is split into
+// hi + lo fp16 (22 bits) after a power-of-two scale that puts its row's largest value at 2^12; keys and queries are exact in one
+// fp16 (8 significant bits, scaled by a power of two per token; what is 2^-24 of a token's largest element or less flushes).
+// Products keep hi*hi + hi*lo + lo*hi, those of the read-out too, whatever the output's type: where q.S and P U cancel, an
+// operand rounded to 11 bits would show in front of bf16's own rounding (it would save 26 of the 578 us).  Against 64 bits a
+// call is 7e-7 off where a binary32 evaluation is 3e-7 off.  The chunk's update is summed in a fresh accumulator and added to S
+// with one rounded fma, so the tensor core's own rounding of running sums does not pile up over a long prompt.
 #pragma once
 #include <cstddef>
 #include <cstdint>
